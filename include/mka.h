@@ -486,7 +486,7 @@ size_t mka_pages_workspace_bytes(int64_t pages, int32_t seqs);
  *   2. Growing sequences take the lowest free pages, in the order of the sequences.  One that grows inside a page that others hold too takes a copy
  *      of it first (its first new page; all that do so in one call copy).  Pages given back in this call by 1 may be taken, by copies not.
  *   From the first sequence on that the free pages do not suffice for, sequences that need pages are left as they are (those that need none are
- *   served); missing (device int32, or NULL) receives how many pages more it would have taken, else 0.
+ *   served); missing (device int32, or NULL) receives how many pages more it would have taken (at most 2^31 - 1), else 0.
  * Table entries behind a sequence's last page are left as they were.  planes: what a copy of a page consists of (at most 8; none: no
  * page is copied, for pools that are never shared).  At most 12288 sequences.
  */

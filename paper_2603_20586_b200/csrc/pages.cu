@@ -31,22 +31,22 @@ template <int kC> __device__ __forceinline__ int of_rank(const int* p, int rank)
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(remote) : "memory");
     return v;
 }
-__device__ __forceinline__ int warp_scan(int x, int lane) {              // sum up to and with this lane
+template <typename T> __device__ __forceinline__ T warp_scan(T x, int lane) {     // sum up to and with this lane
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        const T y = __shfl_up_sync(0xffffffffu, x, o);
         if (lane >= o) x += y;
     }
     return x;
 }
 // Exclusive sum over the CTA's threads, and the total; `sums` [kWarps + 1] in shared memory.
-__device__ __forceinline__ int cta_scan(int x, int* sums, int lane, int warp, int& total) {
-    const int up_to = warp_scan(x, lane);
+template <typename T> __device__ __forceinline__ T cta_scan(T x, T* sums, int lane, int warp, T& total) {
+    const T up_to = warp_scan(x, lane);
     __syncthreads();
     if (lane == 31) sums[warp] = up_to;
     __syncthreads();
     if (warp == 0) {
-        const int own = sums[lane], s = warp_scan(own, lane);
+        const T own = sums[lane], s = warp_scan(own, lane);
         __syncwarp();
         sums[lane] = s - own;
         if (lane == 31) sums[kWarps] = s;
@@ -117,12 +117,15 @@ __device__ __forceinline__ void copy_slice(char* dst, const char* src, int bytes
 // shrinking: 35.9 -> 30.2 us).  Giving back by a kernel over the whole chip in front cost two to seven microseconds and gained one at 500,000 entries.
 __device__ __forceinline__ bool may_resize(const PagesParams& p, int n) { return n >= 0 && (long long)n <= (long long)p.width * p.page_rows; }
 
-struct SeqPlan { int have, grow, first, from; };             // pages it has and takes, the place of its first in the list, the page it has to copy (or -1); grow < 0: left alone
+// What all sequences ask for together may be more than 32 bits hold (2049 tables of 2^20 entries), though no more than `pages` of it is ever served: it is summed in 64,
+// and a place behind the pool's last page is kept as pages + 1.
+struct SeqPlan { int have, grow, first, from; };             // pages it has and takes, the place of its first in the list (< 0: left alone), the page it has to copy (or -1)
 template <int kC>
 __global__ void __launch_bounds__(kThreads) pages_resize_kernel(const PagesParams p, const CopyPagesParams planes, const int slices, const int copy_here) {
     chain_enter();
     extern __shared__ SeqPlan plan[];                        // [seqs]
     __shared__ int sums[kWarps + 1], free_here;
+    __shared__ long long need_sums[kWarps + 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = cluster_rank<kC>();
     const int gw = rank * kWarps + warp;
     constexpr int kAll = kC * kWarps;
@@ -165,7 +168,7 @@ __global__ void __launch_bounds__(kThreads) pages_resize_kernel(const PagesParam
     stretch<kC>(p.pages, rank, warp, first, end);
     uint32_t words[kWords];
     const int mine = count_free(p.refs, first, end, p.pages, lane, words);
-    int need = 0;
+    long long need = 0;
     for (int b0 = 0; b0 < p.seqs; b0 += kThreads) {
         const int s = b0 + tid;
         SeqPlan q = {0, 0, -1, -1};
@@ -173,10 +176,10 @@ __global__ void __launch_bounds__(kThreads) pages_resize_kernel(const PagesParam
             q = plan[s];
             if (q.from >= 0 && __ldcg(p.refs + q.from) <= 1) q.from = -1;             // nobody else holds it
         }
-        const int own = max(q.grow, 0) + (q.from >= 0 ? 1 : 0);
-        int total;
-        const int at = need + cta_scan(own, sums, lane, warp, total);
-        if (s < p.seqs) { plan[s].from = q.from; plan[s].first = q.first < 0 ? -1 : at; }
+        const long long own = max(q.grow, 0) + (q.from >= 0 ? 1 : 0);
+        long long total;
+        const long long at = need + cta_scan(own, need_sums, lane, warp, total);
+        if (s < p.seqs) { plan[s].from = q.from; plan[s].first = q.first < 0 ? -1 : (int)min(at, p.pages + 1LL); }
         need += total;
     }
     int total;
@@ -196,7 +199,7 @@ __global__ void __launch_bounds__(kThreads) pages_resize_kernel(const PagesParam
             if (!(used >> lane & 1) && place < need) p.list[place] = a + lane;
             at += __popc(~used);
         });
-    if (rank == 0 && tid == 0 && p.missing) *p.missing = max(need - all, 0);
+    if (rank == 0 && tid == 0 && p.missing) *p.missing = (int)min(max(need - all, 0LL), 0x7fffffffLL);
     meet<kC>();                                                      // (also: nobody leaves while its shared memory is read)
     auto served = [&](const SeqPlan& q) { const int take = max(q.grow, 0) + (q.from >= 0 ? 1 : 0); return take == 0 || (long long)q.first + take <= all; };
     for (int s = s0; s < p.seqs; s += kAll / per) {
