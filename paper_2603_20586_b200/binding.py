@@ -458,9 +458,9 @@ def mka_pages_compact(planes, refs, table, rows, page_rows: int, refs_out=None, 
 
 
 def mka_l3_index(pool_k, proj, codes=None, stream=None):
-    """Sign-random-projection codes of every (page, KV head) of a key pool [pages, H_kv, page_rows, d] under
+    """Sign-random-projection codes of every (page, KV head) of a bf16 key pool [pages, H_kv, page_rows, d] under
     proj [bits, d] f32; returns int32 [pages, H_kv, bits // 32] holding the code words' bit patterns."""
-    assert pool_k.dim() == 4 and pool_k.stride(3) == 1 and proj.dtype == torch.float32 and proj.is_contiguous()
+    assert pool_k.dtype == torch.bfloat16 and pool_k.dim() == 4 and pool_k.stride(3) == 1 and proj.dtype == torch.float32 and proj.is_contiguous()
     P, H_kv, pr, d = pool_k.shape
     bits = proj.shape[0]
     if codes is None:

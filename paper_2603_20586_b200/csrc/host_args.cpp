@@ -21,6 +21,8 @@
 namespace {
 
 constexpr char kLevelsWanted[] = "levels: tensors [batch, head, row, column] with dense columns, K and V alike; tables and row counts int32";
+constexpr char kTypesWanted[] = "levels: bf16 or f32, all alike";
+constexpr char kPoolsWanted[] = "paged levels: pools of bf16 (8-bit pools have entry points of their own)";
 constexpr char kTensorWanted[] = "a tensor (or None where an argument may be left out) is expected";
 constexpr char kCountWanted[] = "wrong number of arguments";
 struct Bad { const char* what = kLevelsWanted; };    // what an assertion of the binding would have refused
@@ -89,6 +91,12 @@ void check_pair(const at::Tensor& k, const at::Tensor& v) {
     if (v.sizes() != k.sizes()) throw Bad{};
 }
 
+// Rows that the library takes for bf16 or f32 (of `like`'s type, if given): any other type's would be read past their end.
+void check_type(const at::Tensor& k, const at::Tensor& v, const at::Tensor* like = nullptr) {
+    const auto type = (like ? *like : k).scalar_type();
+    if ((type != at::kBFloat16 && type != at::kFloat) || k.scalar_type() != type || v.scalar_type() != type) throw Bad{kTypesWanted};
+}
+
 template <typename F>
 PyObject* guarded(F f) {
     HANDLE_TH_ERRORS
@@ -113,12 +121,15 @@ PyObject* levels(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (n != 2) throw Bad{kCountWanted};
         Seq K(a[0]), V(a[1]);
         int64_t w[18] = {};
+        const at::Tensor* first = nullptr;
         for (int l = 0; l < 3; ++l) {
             const at::Tensor* k = K.tensor_at(l);
             if (!k || k->size(2) == 0) continue;
             const at::Tensor* v = V.tensor_at(l);
             if (!v) throw Bad{};
             check_pair(*k, *v);
+            check_type(*k, *v, first);
+            first = k;
             put_level(w + 6 * l, *k, *v);
         }
         return bytes(w);
@@ -135,6 +146,7 @@ PyObject* grads(PyObject*, PyObject* const* a, Py_ssize_t n) {
             const at::Tensor *dk = dK.tensor_at(l), *dv = dV.tensor_at(l);
             if (!dk || !dv) throw Bad{};
             check_layout(*dk, *dv);
+            check_type(*dk, *dv, k);
             put_level(w + 6 * l, *dk, *dv);
         }
         return bytes(w);
@@ -157,6 +169,7 @@ PyObject* paged_levels(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
             const at::Tensor *v = V.tensor_at(l), *tab = tabs.tensor_at(l), *r = counted ? rows.tensor_at(l) : nullptr;
             if (!v || !tab) throw Bad{};
             check_pair(*k, *v);
+            if (k->scalar_type() != at::kBFloat16 || v->scalar_type() != at::kBFloat16) throw Bad{kPoolsWanted};
             // [B, pages]: one table per sequence; [B, H_kv, pages]: one per (sequence, KV head)
             if (tab->scalar_type() != at::kInt || (tab->dim() != 2 && tab->dim() != 3) || tab->stride(tab->dim() - 1) != 1) throw Bad{};
             if (r && (r->scalar_type() != at::kInt || !r->is_contiguous())) throw Bad{};
@@ -174,6 +187,7 @@ PyObject* paged_level(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (n != 3) throw Bad{kCountWanted};
         const at::Tensor &k = tensor(a[0]), &v = tensor(a[1]), &tab = tensor(a[2]);
         check_layout(k, v);
+        check_type(k, v);
         if (tab.scalar_type() != at::kInt || tab.dim() != 2 || tab.stride(1) != 1) throw Bad{};
         const int64_t w[12] = {address(k), address(v), address(tab), 0, tab.size(1) * k.size(2), tab.stride(0), 0, k.size(2),
                                k.stride(0), k.stride(1), k.stride(2), k.size(0)};
