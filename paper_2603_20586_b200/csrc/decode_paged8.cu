@@ -262,7 +262,10 @@ __global__ void __launch_bounds__(kThreads, 2) decode_paged8_kernel(const __grid
             const int token = kChunk ? (row_first + i / 2 * 8 + 2 * t4 + i % 2) % p8.T : 0;
             place_of[i] = p8.q_offset + token;
 #pragma unroll
-            for (int l = 0; l < 3; ++l) bias[i][l] = log2f(p.gate[((long long)b * (kChunk ? p8.T : 1) + token) * 3 + l]);
+            for (int l = 0; l < 3; ++l) {
+                const float gate = p.gate[((long long)b * (kChunk ? p8.T : 1) + token) * 3 + l];
+                bias[i][l] = gate > 0.f ? log2f(gate) : -INFINITY;             // (NaN closes a level too, as in the tensor-core forward)
+            }
         }
         // of heads 2 t4 and 2 t4 + 1.  m, mv: whole numbers not below the maxima, so that they move only when a maximum passes one
         float m[NB][2], mv[NB][2];
