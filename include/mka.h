@@ -449,8 +449,9 @@ mka_status mka_decode_paged8(const mka_shape* shape, int32_t H_kv, const void* q
  * workspace, exactly, and read from there by the tensor-core forward.  A gate that is not above 0 (NaN included) closes a level for its token.
  * Rows that no token of the call sees (by window, place and row counts; a closed gate hides no NaN) may hold anything; a NaN in a row that some
  * of a sequence's tokens see may show in the others too.
- *   ws: mka_fwd_paged8_workspace_bytes(shape, H_kv, n_level) bytes, 256-byte aligned: partial results, or 4 d bytes for every visible row and KV head, tables, and
- *       the forward's own scratch (mka_fwd_scratch_bytes).  First word: the device status
+ *   ws: mka_fwd_paged8_workspace_bytes(shape, H_kv, n_level) bytes, 256-byte aligned: partial results, or 4 d bytes for every visible row (in pages of 128) and KV head,
+ *       tables, and the forward's own scratch (39 MB, d = 64: 20 MB; without it the forward runs as mka_fwd does without).  That many bytes also serve
+ *       every call that is nowhere larger: in sequences, tokens, q_offset, window and rows of the levels.  First word: the device status
  */
 size_t mka_fwd_paged8_workspace_bytes(const mka_shape* shape, int32_t H_kv, const int64_t n_level[3]);
 mka_status mka_fwd_paged8(const mka_shape* shape, int32_t H_kv, const void* Q, const mka_paged_level8 L[3], const float* gate, void* O,

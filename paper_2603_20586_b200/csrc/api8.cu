@@ -137,16 +137,14 @@ bool chunk8_layout(const mka_shape* s, int H_kv, const int64_t n_level[3], Chunk
     return true;
 }
 
-// The forward's workspace: header | tables | keys and values of the visible rows, level by level | scratch of the forward.
+// The forward's workspace: header | tables | keys and values of the visible rows, level by level | scratch of the forward, as much as is left.
 struct Fwd8Layout {
     int64_t lo[3], hi[3];            // the visible rows of each level
     int first[3], count[3];          // pages of 128 rows that hold visible ones
-    size_t table[3], k[3], v[3], scratch, scratch_bytes, total;
+    size_t table[3], k[3], v[3], scratch;
 };
 bool fwd8_layout(const mka_shape* s, int H_kv, const int64_t n_level[3], Fwd8Layout& w) {
     size_t at = kWsHeader;
-    FwdParams p;
-    memset(&p, 0, sizeof(p));
     if (!visible8(s, n_level, w.lo, w.hi)) return false;
     for (int l = 0; l < 3; ++l) {
         w.first[l] = (int)(w.lo[l] / 128);
@@ -156,13 +154,43 @@ bool fwd8_layout(const mka_shape* s, int H_kv, const int64_t n_level[3], Fwd8Lay
         w.table[l] = at; at += round_up((size_t)s->B * (w.first[l] + w.count[l]) * 4, 256);
         w.k[l] = at; at += bytes;
         w.v[l] = at; at += bytes;
-        p.L[l].n = w.hi[l];
     }
-    p.B = s->B; p.H = s->H; p.T = s->T; p.d = s->d; p.window = s->window; p.q_offset = s->q_offset; p.kv_group = s->H > 0 ? s->H / H_kv : 1;
     w.scratch = at;
-    w.scratch_bytes = fwd_tc_scratch_bytes(p);
-    w.total = at + w.scratch_bytes;
     return true;
+}
+
+// What serves a chunk and every one that is nowhere larger (sequences, tokens, q_offset, window, rows of the levels), whichever way each of them goes.  Neither way's own need
+// grows with every size: the window's rows touch one page more or less by where they lie, partials get fewer where the blocks get more, and a shorter
+// context may go through the single-token kernel where a longer one is expanded.
+size_t fwd8_most(const mka_shape* s, int H_kv, const int64_t n_level[3]) {
+    int64_t lo[3], hi[3], span[3];
+    if (!visible8(s, n_level, lo, hi)) return 0;
+    const int64_t last = (int64_t)s->q_offset + s->T, wide = (int64_t)s->window + s->T - 1;          // rows that windows cover together
+    size_t expand = kWsHeader + fwd_tc_scratch_most(s->d);
+    double mbytes = 0.0;
+    for (int l = 0; l < 3; ++l) {
+        hi[l] = l < 2 && n_level[l] > last ? last : n_level[l];
+        int64_t pages = (hi[l] + 127) / 128;
+        span[l] = hi[l];
+        if (l == 0) {                                        // `wide` rows lie in so many pages at most, and with the rest of a block of 64 in front of them are so many
+            if (pages > (wide + 126) / 128 + 1) pages = (wide + 126) / 128 + 1;
+            if (span[l] > wide + 63) span[l] = wide + 63;
+        }
+        if ((int64_t)s->B * pages > 0x7fffffffLL) return 0;
+        expand += round_up((size_t)s->B * ((hi[l] + 127) / 128) * 4, 256) + 2 * (size_t)s->B * pages * H_kv * 128 * s->d * 2;
+        mbytes += (double)span[l] * s->B * H_kv * (2e-6 * s->d);
+    }
+    const int64_t rows = s->H / H_kv * (int64_t)s->T;
+    size_t walk = kWsHeader;
+    for (int64_t b = 1; 16 * (b - 1) < rows && 16 * (b - 1) < kMaxChunkRows && b * H_kv <= 65535; ++b) {
+        const int64_t here = 16 * b < rows ? 16 * b : rows;
+        const size_t bytes = kWsHeader + (size_t)s->B * H_kv * here * (size_t)decode8_slots(span, (int)(b * H_kv), s->d) * (s->d + 2) * sizeof(float);
+        if (bytes > walk) walk = bytes;
+    }
+    const int64_t blocks = (rows + 15) / 16;
+    const bool all_walk = rows <= kMaxChunkRows && blocks * H_kv <= 65535 && (int64_t)s->B * s->H * s->T <= 0x7fffffffLL && last <= 0x7fffffffLL &&
+                          (rows == 0 || walk_in_blocks(s->d, blocks, s->H / H_kv, mbytes));
+    return all_walk || walk > expand ? walk : expand;
 }
 
 mka_status check_tables(const mka_page_tables* t) {
@@ -304,11 +332,8 @@ static mka_status run_chunk8(const mka_shape* s, int32_t H_kv, const void* Q, co
 }
 
 size_t mka_fwd_paged8_workspace_bytes(const mka_shape* s, int32_t H_kv, const int64_t n_level[3]) {
-    Fwd8Layout w;
-    Chunk8 c;
-    if (!n_level || check_shape8(s, H_kv, false) != MKA_OK || !chunk8_layout(s, H_kv, n_level, c)) return 0;
-    if (c.blocks) return c.total;
-    return fwd8_layout(s, H_kv, n_level, w) ? w.total : 0;
+    if (!n_level || check_shape8(s, H_kv, false) != MKA_OK) return 0;
+    return fwd8_most(s, H_kv, n_level);
 }
 
 mka_status mka_fwd_paged8(const mka_shape* s, int32_t H_kv, const void* Q, const mka_paged_level8 L[3], const float* gate, void* O, float* LSE,
@@ -329,7 +354,7 @@ mka_status mka_fwd_paged8(const mka_shape* s, int32_t H_kv, const void* Q, const
     }
     Fwd8Layout w;
     if (!fwd8_layout(s, H_kv, n_level, w)) return MKA_ERR_SHAPE;
-    if (!ws || ws_bytes < w.total) return MKA_ERR_WORKSPACE;
+    if (!ws || ws_bytes < w.scratch) return MKA_ERR_WORKSPACE;
     if ((double)((s->T + 127LL) / 128) * s->H * s->B > 2147483647.0) return MKA_ERR_SHAPE;     // the kernel numbers its blocks in an int
     char* const base = static_cast<char*>(ws);
     Expand8Params x;
@@ -360,7 +385,7 @@ mka_status mka_fwd_paged8(const mka_shape* s, int32_t H_kv, const void* Q, const
     p.B = s->B; p.H = s->H; p.T = s->T; p.d = s->d;
     p.window = s->window; p.q_offset = s->q_offset; p.scale = resolve_scale(s);
     p.mode = s->mode; p.kv_group = s->H / H_kv; p.paged = P;
-    if (w.scratch_bytes) { p.scratch = base + w.scratch; p.scratch_bytes = w.scratch_bytes; }
+    if (ws_bytes > w.scratch) { p.scratch = base + w.scratch; p.scratch_bytes = ws_bytes - w.scratch; }
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     cudaError_t e = launch_expand8(x, cs);
     if (e == cudaSuccess) e = launch_fwd_tc(p, static_cast<unsigned int*>(ws), cs);

@@ -297,6 +297,7 @@ bool bwd_tc_eligible(const BwdParams& p, int dtype);
 // Tensor-core (TMA + tcgen05) forward; returns cudaErrorNotSupported when the shape is not eligible.
 cudaError_t launch_fwd_tc(const FwdParams& p, unsigned int* status_word, cudaStream_t st);
 bool fwd_tc_eligible(const FwdParams& p, int dtype);
+size_t fwd_tc_scratch_most(int d);                    // no call of that width has use for more
 size_t fwd_tc_scratch_bytes(const FwdParams& p);      // scratch with which the call would run faster, 0: none
 
 }  // namespace mka

@@ -1228,6 +1228,10 @@ cudaError_t launch_t(const FwdParams& fp, unsigned int* status_word, cudaStream_
 
 }  // namespace
 
+size_t fwd_tc_scratch_most(int d) {
+    const size_t slots = d == 128 ? (size_t)Cfg<128>::kSlotFloats * Cfg<128>::kCtasPerSm : (size_t)Cfg<64>::kSlotFloats * Cfg<64>::kCtasPerSm;
+    return 2 * 148 * slots * sizeof(float);
+}
 size_t fwd_tc_scratch_bytes(const FwdParams& p) {
     if (p.B == 0 || p.H == 0 || p.T == 0) return 0;
     return p.d == 128 ? scratch_bytes_t<128>(p) : scratch_bytes_t<64>(p);
