@@ -433,8 +433,9 @@ mka_status mka_append_kv_paged8(int32_t B, int32_t H, int64_t n, int32_t d, int3
 
 /*
  * mka_decode_paged over 8-bit levels: the same result as on the levels' values.  q, O bf16; d = 64 or 128; at most 16 query heads per KV head.
- * Codes become f16 in registers, exactly; queries (scaled by a power of two per row) and weights are f16 in the products, sums fp32.  A weight is off by 2^-11 of itself,
- * and by 2^-38 of the largest product of a weight and a value block's scale: far below what a rounding of that block's codes makes.
+ * Codes become f16 in registers, exactly; queries (scaled by a power of two per row) and weights are f16 in the products, sums fp32.  A weight (times its
+ * value block's scale) is off by 2^-11 of itself, and by 2^-34 of the largest such product of the row; where the exponents of the value blocks lie D > 91 apart, by
+ * 2^(D - 125) of it, 2^-29 at most: far below what a rounding of that block's codes makes.
  * A NaN among a sequence's valid keys, or an infinite score, gives NaN in O (LSE +inf).
  *   ws: mka_decode_paged8_workspace_bytes(shape, H_kv, n_level) bytes, 4-byte aligned; first word: the device status (bounded waits as in
  *       mka_decode_paged)

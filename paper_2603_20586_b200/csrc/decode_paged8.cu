@@ -20,8 +20,9 @@
 // Ranges: f16 has the precision for codes (exact), queries (8 bits) and weights (11 bits), but not the range.  Every query row is scaled by the power of two
 // that brings its largest element to 2^14 .. 2^15; what falls below f16's smallest number then is 2^-39 of that.  The keys' exponent and the row's
 // factor are applied to the scores in fp32.  Weights enter the second product as p 2^ev / 2^mv with mv the running maximum of (group maximum of
-// log2 p) + ev over the row groups, at 2^14 the largest: a weight is lost only where its whole block counts 2^-38 of the largest, whatever the exponents of
-// the blocks are.  Maximum, sum of the weights and accumulators are fp32, each row's accumulator in units of 2^(mv - 14).
+// log2 p) + ev over the row groups, at 2^14 the largest.  An f16 below 2^-14 is off by up to 2^-25, which is 2^-39 of 2^mv; mv lies less than 5 above the largest real product
+// (4 where a tile's exponents lie up to 4 apart, 1 as it is a whole number): 2^-34 of that.  p itself, and a warp's or a share's whole state, counts as 0 below 2^-125 of the
+// largest weight: at exponents D apart, 2^(D - 125) of the largest product, which is more only from D = 92 on (2^-29 at D = 96).  Maximum, sum of the weights and accumulators are fp32, each row's accumulator in units of 2^(mv - 14).
 #include <cuda_fp16.h>
 
 #include <type_traits>
