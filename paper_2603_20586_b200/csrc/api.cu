@@ -339,11 +339,15 @@ static mka_status paged_plan(const int64_t n_level[3], int32_t B, int32_t H_kv, 
     return MKA_OK;
 }
 
+static int64_t dealt_tiles(const int64_t n_level[3]) {
+    int64_t tiles = 0;
+    for (int l = 0; l < 3; ++l) tiles += (n_level[l] + 63) / 64;
+    return tiles;
+}
 // Entries per query head of the copy-engine form: a count, and one partial for every share that a list can touch.  The H_kv lists
 // of one sequence are equally long, so a share (all tiles / 296, at least two) is no less than H_kv / 296 of a list.
 static int64_t dealt_slots(const int64_t n_level[3], int32_t H_kv) {
-    int64_t tiles = 0;
-    for (int l = 0; l < 3; ++l) tiles += (n_level[l] + 63) / 64;
+    const int64_t tiles = dealt_tiles(n_level);
     const int64_t by_share = kDealCtas / H_kv + 2, by_list = tiles / 2 + 2;
     return 1 + (by_share < by_list ? by_share : by_list);
 }
@@ -359,7 +363,7 @@ static mka_status run_decode_paged(DecodePagedParams& p, DecodeParams& c, const 
                                    cudaStream_t cs) {
     p.chunk_rows = plan.chunk_rows; p.total_chunks = plan.total_chunks;
     for (int l = 0; l < 3; ++l) { p.n_chunks[l] = plan.n_chunks[l]; c.n_chunks[l] = plan.n_chunks[l]; }
-    if (plan.total_chunks > 0 && decode_paged_dealt(p)) {
+    if (plan.total_chunks > 0 && decode_paged_dealt(p) && deal_fits(p.B, p.H_kv, dealt_tiles(n_level))) {
         p.dealt = c.counted = 1;
         c.expected = kDealCtas / (p.B * p.H_kv) + 1;
         p.total_chunks = dealt_slots(n_level, p.H_kv);

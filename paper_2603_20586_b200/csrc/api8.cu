@@ -59,9 +59,13 @@ mka_status status_of(cudaError_t e) { return e == cudaSuccess ? MKA_OK : (e == c
 
 // Entries per query head of the decode's partials: a count, and one for every share that a list can touch.  The H_kv lists of one sequence are
 // equally long, so a share (all tiles / 296, at least two) is no less than H_kv / 296 of a list.
-int64_t decode8_slots(const int64_t n_level[3], int32_t H_kv, int32_t d) {
+int64_t decode8_tiles(const int64_t n_level[3], int32_t d) {
     int64_t tiles = 0;
     for (int l = 0; l < 3; ++l) tiles += (n_level[l] + tile_rows8(d) - 1) / tile_rows8(d);
+    return tiles;
+}
+int64_t decode8_slots(const int64_t n_level[3], int32_t H_kv, int32_t d) {
+    const int64_t tiles = decode8_tiles(n_level, d);
     const int64_t by_share = kDealCtas / H_kv + 2, by_list = tiles / 2 + 2;
     return 1 + (by_share < by_list ? by_share : by_list);
 }
@@ -131,7 +135,7 @@ bool chunk8_layout(const mka_shape* s, int H_kv, const int64_t n_level[3], Chunk
     c.lo = lo[0];
     double mbytes = 0.0;                                     // of codes that the chunk sees
     for (int l = 0; l < 3; ++l) mbytes += (double)span[l] * s->B * H_kv * (2e-6 * s->d);
-    if (!walk_in_blocks(s->d, blocks, s->H / H_kv, mbytes)) return true;
+    if (!walk_in_blocks(s->d, blocks, s->H / H_kv, mbytes) || !deal_fits(s->B, blocks * H_kv, decode8_tiles(span, s->d))) return true;
     c.blocks = (int)blocks;
     c.total = kWsHeader + (size_t)s->B * s->H * s->T * (size_t)decode8_slots(span, (int)(blocks * H_kv), s->d) * (s->d + 2) * sizeof(float);
     return true;
@@ -189,7 +193,7 @@ size_t fwd8_most(const mka_shape* s, int H_kv, const int64_t n_level[3]) {
     }
     const int64_t blocks = (rows + 15) / 16;
     const bool all_walk = rows <= kMaxChunkRows && blocks * H_kv <= 65535 && (int64_t)s->B * s->H * s->T <= 0x7fffffffLL && last <= 0x7fffffffLL &&
-                          (rows == 0 || walk_in_blocks(s->d, blocks, s->H / H_kv, mbytes));
+                          (rows == 0 || (walk_in_blocks(s->d, blocks, s->H / H_kv, mbytes) && deal_fits(s->B, blocks * H_kv, decode8_tiles(span, s->d))));
     return all_walk || walk > expand ? walk : expand;
 }
 
@@ -274,6 +278,7 @@ mka_status mka_decode_paged8(const mka_shape* s, int32_t H_kv, const void* q, co
     if (!q || !gate || !O) return MKA_ERR_ARG;
     if (!aligned(q, 16) || !aligned(O, 16) || !aligned(ws, 4)) return MKA_ERR_ALIGN;
     const int64_t n_level[3] = {L[0].n, L[1].n, L[2].n};
+    if (!deal_fits(s->B, H_kv, decode8_tiles(n_level, s->d))) return MKA_ERR_SHAPE;
     if (!ws || ws_bytes < mka_decode_paged8_workspace_bytes(s, H_kv, n_level)) return MKA_ERR_WORKSPACE;
     DecodePaged8Params p;
     memset(&p, 0, sizeof(p));

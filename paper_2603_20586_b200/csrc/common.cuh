@@ -168,6 +168,11 @@ struct DecodePagedParams {
     int skip[3];                       // rows of each level in front of a list (several tokens: what the first one's window leaves out)
 };
 constexpr int kDealCtas = 148 * 2;     // CTAs of the copy-engine form: two per SM
+// Whether the dealing (tile_deal.cuh) can number the tiles: those of one list of every sequence, those of one sequence's lists, and a CTA's share, in 32 bits.
+// `tiles`: the most that a list has.
+inline bool deal_fits(long long B, long long H_kv, long long tiles) {
+    return tiles * B <= 0x7fffffffLL && tiles * H_kv <= 0x7fffffffLL && (double)tiles * (double)B * (double)H_kv / kDealCtas < 2147483646.0;
+}
 bool decode_paged_dealt(const DecodePagedParams& p);
 cudaError_t launch_decode_paged(const DecodePagedParams& p, cudaStream_t st);
 
