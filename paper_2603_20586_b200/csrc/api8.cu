@@ -202,14 +202,14 @@ mka_status check_tables(const mka_page_tables* t) {
     if (t->pages < 0 || t->pages > 0x7fffff00LL || t->seqs < 0 || t->width < 0 || t->width > 0x7ff00000 || t->table_stride < t->width || t->page_rows <= 0) return MKA_ERR_SHAPE;
     return MKA_OK;
 }
-mka_status check_planes(const mka_page_plane* planes, int n, CopyPagesParams& c) {
+mka_status check_planes(const mka_page_plane* planes, int n, int64_t pages, CopyPagesParams& c) {
     if (n < 0 || n > kMaxPlanes) return MKA_ERR_SHAPE;
     if (n > 0 && !planes) return MKA_ERR_ARG;
     memset(&c, 0, sizeof(c));
     for (int j = 0; j < n; ++j) {
         const mka_page_plane& x = planes[j];
         if (x.heads < 0 || x.bytes < 0 || x.stride_page < 0 || x.stride_h < 0) return MKA_ERR_SHAPE;
-        if (x.heads == 0 || x.bytes == 0) continue;
+        if (x.heads == 0 || x.bytes == 0 || pages == 0) continue;
         if (!x.base) return MKA_ERR_ARG;
         c.plane[c.planes++] = {static_cast<char*>(x.base), x.stride_page, x.stride_h, x.heads, x.bytes};
     }
@@ -408,7 +408,7 @@ mka_status mka_pages_resize(const mka_page_tables* t, const mka_page_plane* plan
     mka_status st = check_tables(t);
     if (st != MKA_OK) return st;
     CopyPagesParams c;
-    if ((st = check_planes(planes, n_planes, c)) != MKA_OK) return st;
+    if ((st = check_planes(planes, n_planes, t->pages, c)) != MKA_OK) return st;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     if (t->seqs == 0) return missing && cudaMemsetAsync(missing, 0, 4, cs) != cudaSuccess ? MKA_ERR_CUDA : MKA_OK;
     if (t->seqs > kMaxSeqs) return MKA_ERR_SHAPE;
@@ -440,11 +440,12 @@ mka_status mka_pages_compact(const mka_page_tables* t, const mka_page_plane* pla
     mka_status st = check_tables(t);
     if (st != MKA_OK) return st;
     CopyPagesParams c;
-    if ((st = check_planes(planes, n_planes, c)) != MKA_OK) return st;
+    if ((st = check_planes(planes, n_planes, t->pages, c)) != MKA_OK) return st;
     if (table_out_stride < t->width) return MKA_ERR_SHAPE;
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
-    if (t->pages == 0) return live && cudaMemsetAsync(live, 0, 4, cs) != cudaSuccess ? MKA_ERR_CUDA : MKA_OK;
-    if (!t->refs || !refs_out || !remap) return MKA_ERR_ARG;
+    const bool tables = t->seqs > 0 && t->width > 0;         // (of an empty pool too: table_out receives their entries as they are)
+    if (t->pages == 0 && !tables) return live && cudaMemsetAsync(live, 0, 4, cs) != cudaSuccess ? MKA_ERR_CUDA : MKA_OK;
+    if (t->pages > 0 && (!t->refs || !refs_out || !remap)) return MKA_ERR_ARG;
     if (t->seqs > 0 && (!t->rows || (t->width > 0 && (!t->table || !table_out)))) return MKA_ERR_ARG;
     if (!aligned(ws, 4)) return MKA_ERR_ALIGN;
     if (!ws || ws_bytes < mka_pages_workspace_bytes(t->pages, t->seqs)) return MKA_ERR_WORKSPACE;
