@@ -201,6 +201,27 @@ def _stream(stream) -> int:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
 
 
+def _torch_stream(stream, device):
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device)
+
+
+def _on(stream, *own):
+    """Tensors that a call made on torch's current stream for its work on another one: when they are dropped, their memory is not given out again before
+    that stream is done with them."""
+    if stream is not None:
+        for t in own:
+            if t is not None and t.is_cuda:
+                t.record_stream(_torch_stream(stream, t.device))
+
+
+def _scratch(nbytes: int, device, stream) -> torch.Tensor:
+    """nbytes of torch's memory on the call's stream, to which it goes back when the call has been queued there."""
+    if stream is None or torch.device(device).type != "cuda":
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with torch.cuda.stream(_torch_stream(stream, device)):
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
 def _n_level(n) -> ctypes.Array:
     return (ctypes.c_int64 * 3)(*[int(x) for x in n])
 
@@ -258,12 +279,13 @@ def mka_router(R: torch.Tensor, W_r: torch.Tensor, b_r: Optional[torch.Tensor], 
     assert R.is_contiguous() and W_r.is_contiguous() and W_r.dtype == torch.float32 and W_r.shape == (D, 3)
     if gate is None:
         gate = _empty_f32(R, R.dim() - 1, 3)
+        _on(stream, gate)
     _check(_host_args.call_router(_router, R, W_r, b_r, rows, D, _dt(R), route, gate, log2_gate, route_idx, _stream(stream)), "mka_router")
     return gate
 
 
-def alloc_workspace(shape: mka_shape, n_level, which: int, device) -> torch.Tensor:
-    return torch.empty(mka_workspace_bytes(shape, n_level, which), dtype=torch.uint8, device=device)
+def alloc_workspace(shape: mka_shape, n_level, which: int, device, stream=None) -> torch.Tensor:
+    return _scratch(mka_workspace_bytes(shape, n_level, which), device, stream)
 
 
 def _fwd_scratch(shape: mka_shape, H_kv: int, n_level, device, stream) -> Optional[torch.Tensor]:
@@ -275,11 +297,7 @@ def _fwd_scratch(shape: mka_shape, H_kv: int, n_level, device, stream) -> Option
     if nbytes == 0:
         return None
     try:
-        if stream is None:
-            return torch.empty(nbytes, dtype=torch.uint8, device=device)
-        # from the allocator's blocks of that stream, to which it goes back when the call has been queued there
-        with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device)):
-            return torch.empty(nbytes, dtype=torch.uint8, device=device)
+        return _scratch(nbytes, device, stream)
     except torch.OutOfMemoryError:                                           # the call runs without, as it would have
         return None
 
@@ -292,11 +310,13 @@ def mka_fwd(shape: mka_shape, Q, K, V, gate, O=None, LSE=None, ws=None, stream=N
     assert Q.is_contiguous() and gate.is_contiguous() and gate.dtype == torch.float32
     if O is None:
         O = _empty_like(Q)
+        _on(stream, O)
     if LSE is None and want_lse and shape.mode == MKA_MODE_FAST:
         LSE = _empty_f32(Q, 3, 0)
+        _on(stream, LSE)
     n = _row_counts(K)
     if ws is None:
-        ws = alloc_workspace(shape, n, MKA_WS_FWD, Q.device)
+        ws = alloc_workspace(shape, n, MKA_WS_FWD, Q.device, stream)
     tmp = _fwd_scratch(shape, 0, n, Q.device, stream)
     _check(_host_args.call_fwd(_fwd, shape, Q, _levels(K, V), gate, O, LSE, ws, ws.numel(), tmp, 0 if tmp is None else tmp.numel(),
                                _stream(stream)), "mka_fwd")
@@ -307,10 +327,12 @@ def mka_decode(shape: mka_shape, q, K, V, gate, O=None, LSE=None, ws=None, strea
     assert q.is_contiguous() and gate.is_contiguous() and gate.dtype == torch.float32
     if O is None:
         O = torch.empty_like(q)
+        _on(stream, O)
     if LSE is None:
         LSE = _empty_f32(q, 2, 0)
+        _on(stream, LSE)
     if ws is None:
-        ws = alloc_workspace(shape, [0 if k is None else k.shape[2] for k in K], MKA_WS_DECODE, q.device)
+        ws = alloc_workspace(shape, [0 if k is None else k.shape[2] for k in K], MKA_WS_DECODE, q.device, stream)
     _check(_host_args.call_decode(_decode, shape, q, _levels(K, V), gate, O, LSE, ws, ws.numel(), _stream(stream)), "mka_decode")
     return O, LSE
 
@@ -338,10 +360,12 @@ def mka_fwd_paged(shape: mka_shape, H_kv: int, Q, pools_k, pools_v, tables, n, g
     B, H, T, d = Q.shape
     if O is None:
         O = torch.empty_like(Q)
+        _on(stream, O)
     if LSE is None:
         LSE = _empty_f32(Q, 3, 0)
+        _on(stream, LSE)
     if ws is None:
-        ws = torch.zeros(256, dtype=torch.uint8, device=Q.device)
+        ws = _scratch(256, Q.device, stream)
     tmp = None
     if rows is None or not any(r is not None for r in rows):
         tmp = _fwd_scratch(shape, H_kv, [0 if pools_k[l] is None else int(n[l]) for l in range(3)], Q.device, stream)
@@ -361,10 +385,12 @@ def mka_decode_paged(shape: mka_shape, H_kv: int, q, pools_k, pools_v, tables, n
     assert q.is_contiguous() and gate.is_contiguous() and gate.dtype == torch.float32
     if O is None:
         O = torch.empty_like(q)
+        _on(stream, O)
     if LSE is None:
         LSE = _empty_f32(q, 2, 0)
+        _on(stream, LSE)
     if ws is None:
-        ws = torch.empty(mka_decode_paged_workspace_bytes(shape, H_kv, n), dtype=torch.uint8, device=q.device)
+        ws = _scratch(mka_decode_paged_workspace_bytes(shape, H_kv, n), q.device, stream)
     _check(_host_args.call_decode_paged(_decode_paged, shape, H_kv, q, _paged_levels(pools_k, pools_v, tables, rows, n), gate, O, LSE, ws, ws.numel(),
                                         _stream(stream)), "mka_decode_paged")
     return O, LSE
@@ -374,14 +400,6 @@ def mka_decode_paged(shape: mka_shape, H_kv: int, q, pools_k, pools_v, tables, n
 
 
 _device = torch._C._cuda_getDevice      # the calls below run on the current device, and the native code holds their tensors to it
-
-
-def _scratch(nbytes: int, like: torch.Tensor, stream) -> torch.Tensor:
-    """nbytes of torch's memory on the call's stream, to which it goes back when the call has been queued there."""
-    if stream is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
-    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, like.device)):
-        return torch.empty(nbytes, dtype=torch.uint8, device=like.device)
 
 
 def mka_append_kv_paged8(K, V, pool_k, pool_v, exp_k, exp_v, table, dst_offset=0, dst_offsets=None, stream=None):
@@ -403,10 +421,12 @@ def mka_fwd_paged8_workspace_bytes(shape: mka_shape, H_kv: int, n) -> int:
 def _attend8(call, where, size, shape, H_kv, q, pools_k, pools_v, exps_k, exps_v, tables, n, gate, rows, O, LSE, ws, stream):
     if O is None:
         O = _empty_like(q)
+        _on(stream, O)
     if LSE is None:
         LSE = _empty_f32(q, q.dim() - 1, 0)
+        _on(stream, LSE)
     if ws is None:
-        ws = _scratch(size(shape, H_kv, [0 if pools_k[l] is None else n[l] for l in range(3)]), q, stream)
+        ws = _scratch(size(shape, H_kv, [0 if pools_k[l] is None else n[l] for l in range(3)]), q.device, stream)
     _check(_host_args.attend8(call, _device(), shape, H_kv, q, pools_k, pools_v, exps_k, exps_v, tables, rows, n, gate, O, LSE, ws, _stream(stream)), where)
     return O, LSE
 
@@ -437,7 +457,7 @@ def mka_pages_resize(planes, refs, table, rows, new_rows, page_rows: int, missin
     ones and a copy of a last page that others hold too.  refs int32 [pages], table int32 [seqs, width], rows int32 [seqs], all updated; planes: the
     cache's tensors [pages, ...] (none: no page is copied); missing int32 [1]: how many pages too few there were."""
     if ws is None:
-        ws = _scratch(mka_pages_workspace_bytes(refs.numel(), rows.numel()), refs, stream)
+        ws = _scratch(mka_pages_workspace_bytes(refs.numel(), rows.numel()), refs.device, stream)
     _check(_host_args.pages_resize(_resize, _device(), planes, refs, table, rows, new_rows, page_rows, missing, ws, _stream(stream)), "mka_pages_resize")
 
 
@@ -449,9 +469,11 @@ def mka_pages_fork(refs, table, rows, parents, children, page_rows: int, stream=
 def mka_pages_compact(planes, refs, table, rows, page_rows: int, refs_out=None, table_out=None, remap=None, live=None, ws=None, stream=None):
     """Moves the pages in use to the front of the pool.  refs_out and table_out (default: refs and table themselves) receive the counts and tables after
     it, remap int32 [pages] where every page went (-1: free), live int32 [1] how many are in use.  Returns remap."""
-    remap = _empty_like(refs) if remap is None else remap
+    if remap is None:
+        remap = _empty_like(refs)
+        _on(stream, remap)
     if ws is None:
-        ws = _scratch(mka_pages_workspace_bytes(refs.numel(), rows.numel()), refs, stream)
+        ws = _scratch(mka_pages_workspace_bytes(refs.numel(), rows.numel()), refs.device, stream)
     _check(_host_args.pages_compact(_compact, _device(), planes, refs, table, rows, page_rows, refs if refs_out is None else refs_out,
                                     table if table_out is None else table_out, remap, live, ws, _stream(stream)), "mka_pages_compact")
     return remap
@@ -465,6 +487,7 @@ def mka_l3_index(pool_k, proj, codes=None, stream=None):
     bits = proj.shape[0]
     if codes is None:
         codes = torch.empty(P, H_kv, bits // 32, dtype=torch.int32, device=pool_k.device)
+        _on(stream, codes)
     _check(lib.mka_l3_index(_ptr(pool_k), P, H_kv, pr, d, pool_k.stride(0), pool_k.stride(1), pool_k.stride(2), _ptr(proj),
                             bits, _ptr(codes), _stream(stream)), "mka_l3_index")
     return codes
@@ -478,10 +501,13 @@ def mka_l3_retrieve(q, H_kv: int, proj, codes, bank, bank_len, R: int, page_rows
     B, H, d = q.shape
     if table is None:
         table = torch.empty(B, H_kv, R, dtype=torch.int32, device=q.device)
+        _on(stream, table)
     if n_sel is None:
         n_sel = torch.empty(B, dtype=torch.int32, device=q.device)
+        _on(stream, n_sel)
     if rows is None:
         rows = torch.empty(B, dtype=torch.int32, device=q.device)
+        _on(stream, rows)
     _check(lib.mka_l3_retrieve(_ptr(q), B, H, H_kv, d, _ptr(proj), proj.shape[0], _ptr(codes), _ptr(bank), _ptr(bank_len),
                                bank.stride(0), bank.shape[1], R, page_rows, _ptr(table), _ptr(n_sel), _ptr(rows),
                                _stream(stream)), "mka_l3_retrieve")
@@ -509,21 +535,27 @@ def mka_bwd(shape: mka_shape, Q, K, V, gate, O, LSE, dO, R=None, dQ=None, dK=Non
     dev = Q.device
     if dQ is None:
         dQ = torch.empty_like(Q)
+        _on(stream, dQ)
     if dK is None:
         dK = _host_args.empties_like(K)
+        _on(stream, *dK)
     if dV is None:
         dV = _host_args.empties_like(V)
+        _on(stream, *dV)
     if dG is None:
         dG = _empty_f32(gate, gate.dim(), 0)
+        _on(stream, dG)
     if R is not None and want_router_grad:
         assert R.is_contiguous()
         if dW_r is None:
             dW_r = torch.empty((R.shape[-1], 3), dtype=torch.float32, device=dev)
+            _on(stream, dW_r)
         if db_r is None:
             db_r = torch.empty((3,), dtype=torch.float32, device=dev)
+            _on(stream, db_r)
     grads = _host_args.grads(K, dK, dV)
     if ws is None:
-        ws = alloc_workspace(shape, [0 if k is None else k.shape[2] for k in K], MKA_WS_BWD, dev)
+        ws = alloc_workspace(shape, [0 if k is None else k.shape[2] for k in K], MKA_WS_BWD, dev, stream)
     _check(_host_args.call_bwd(_bwd, shape, Q, _levels(K, V), gate, O, LSE, dO, R, _dt(R) if R is not None else MKA_F32, dQ, grads, dG, dW_r,
                                db_r, ws, ws.numel(), _stream(stream)), "mka_bwd")
     return {"dQ": dQ, "dK": dK, "dV": dV, "dG": dG, "dW_r": dW_r, "db_r": db_r}
@@ -541,8 +573,10 @@ def mka_fuse_kv(K, V, gate, out_k=None, out_v=None, dst_offset=0, stream=None):
     assert gate.is_contiguous() and gate.dtype == torch.float32 and tuple(gate.shape) == (B, n, 3)
     if out_k is None:
         out_k = torch.empty((B, H, dst_offset + n, d), dtype=ref.dtype, device=ref.device)
+        _on(stream, out_k)
     if out_v is None:
         out_v = torch.empty_like(out_k)
+        _on(stream, out_v)
     assert out_k.stride(3) == 1 and out_v.stride() == out_k.stride() and out_k.dtype == ref.dtype
     dst = mka_level_grad(out_k.data_ptr(), out_v.data_ptr(), out_k.shape[2], out_k.stride(0), out_k.stride(1), out_k.stride(2))
     _check(lib.mka_fuse_kv(B, H, n, d, _dt(ref), _levels(K, V), _ptr(gate), ctypes.byref(dst), dst_offset, _stream(stream)),
@@ -569,6 +603,7 @@ def mka_l2_summary(X, kind=MKA_SUMMARY_MEAN, beta=0.9, state=None, n_prev=0, M2=
     B, T, D = X.shape
     if M2 is None:
         M2 = torch.empty_like(X)
+        _on(stream, M2)
     assert M2.is_contiguous() and M2.dtype == X.dtype
     if state is not None:
         assert state.is_contiguous() and state.dtype == torch.float32 and tuple(state.shape) == (B, D)
