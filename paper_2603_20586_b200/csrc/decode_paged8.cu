@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, 2) decode_paged8_kernel(const __grid
 #pragma unroll
             for (int l = 0; l < 3; ++l) {
                 const float gate = p.gate[((long long)b * (kChunk ? p8.T : 1) + token) * 3 + l];
-                bias[i][l] = gate > 0.f ? log2f(gate) : -INFINITY;             // (NaN closes a level too, as in the tensor-core forward)
+                bias[i][l] = log2f(kChunk ? fmaxf(gate, 0.f) : gate);          // (negative ones and NaN close a level too, as in the tensor-core forward)
             }
         }
         // of heads 2 t4 and 2 t4 + 1.  m, mv: whole numbers not below the maxima, so that they move only when a maximum passes one
