@@ -449,8 +449,8 @@ mka_status mka_decode_paged8(const mka_shape* shape, int32_t H_kv, const void* q
  * mka_fwd_paged over 8-bit levels (a chunk of a prompt against the cache, or the few tokens of a draft): the same result as on the levels' values.  Few tokens go
  * through the kernel of mka_decode_paged8, heads x tokens in blocks of sixteen; for more the rows that the chunk can see are expanded to bf16 in the
  * workspace, exactly, and read from there by the tensor-core forward.  A gate that is not above 0 (NaN included) closes a level for its token.
- * Rows that no token of the call sees (by window, place and row counts; a closed gate hides no NaN) may hold anything; a NaN in a row that some
- * of a sequence's tokens see may show in the others too.
+ * Rows that no token of the call sees (by window, place and row counts; a closed gate hides no NaN) may hold anything; a NaN value in a row that some
+ * of a sequence's tokens see may show in the others too.  A score of NaN or +inf ends its row as O = 0, LSE = -inf, as in mka_fwd.
  *   ws: mka_fwd_paged8_workspace_bytes(shape, H_kv, n_level) bytes, 256-byte aligned: partial results, or 4 d bytes for every visible row (in pages of 128) and KV head,
  *       tables, and the forward's own scratch (39 MB, d = 64: 20 MB; without it the forward runs as mka_fwd does without).  That many bytes also serve
  *       every call that is nowhere larger: in sequences, tokens, q_offset, window and rows of the levels.  First word: the device status

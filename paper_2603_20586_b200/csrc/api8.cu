@@ -329,6 +329,7 @@ static mka_status run_chunk8(const mka_shape* s, int32_t H_kv, const void* Q, co
     c.O = O; c.LSE = LSE; c.gate = gate; c.B = s->B; c.H = p.base.H; c.d = s->d;
     c.partial = p.base.partial; c.total_chunks = any ? p.base.total_chunks : 0; c.counted = any ? 1 : 0;
     c.expected = (int)(kDealCtas / ((int64_t)s->B * p.base.H_kv)) + 1;
+    c.nan_is_none = 1;
     if (!any) c.status = p.base.status;
     p.O = O; p.LSE = LSE;
     cudaError_t e = any ? launch_chunk_paged8(p, cs) : cudaSuccess;

@@ -135,6 +135,7 @@ struct DecodeParams {
     float* partial;      // [B*H, total_chunks, d+2]
     int counted;         // combine: entry 0 of a (batch, head) holds the number of partials that follow, which carry the gate already
     int expected;        // counted: partials of a (batch, head) in a batch of equal lengths
+    int nan_is_none;     // combine: a row with an infinite sum (a score of NaN or +inf) ends as one that sees nothing, as in the tensor-core forward
     unsigned int* status;   // device status word that the combine kernel sets to MKA_OK, or null (kernels before it may wait and set it)
 };
 cudaError_t launch_decode(const DecodeParams& p, cudaStream_t st);

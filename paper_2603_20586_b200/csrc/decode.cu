@@ -399,9 +399,10 @@ __global__ void __launch_bounds__(DH * GROUPS) decode_combine_kernel(const Decod
 #pragma unroll
     for (int g = 1; g < GROUPS; ++g) A += sa[g - 1][col];
     __nv_bfloat16* O = static_cast<__nv_bfloat16*>(p.O) + bh * DH;
-    O[col] = __float2bfloat16_rn(Z > 0.f ? A / Z : 0.f);
+    const bool some = Z > 0.f && !(p.nan_is_none && Z == INFINITY);
+    O[col] = __float2bfloat16_rn(some ? A / Z : 0.f);
     if (p.status && bh == 0 && tid == 0) *p.status = MKA_OK;
-    if (p.LSE && tid == 0) p.LSE[bh] = Z > 0.f ? (M + log2f(Z)) * kLn2 : -INFINITY;
+    if (p.LSE && tid == 0) p.LSE[bh] = some ? (M + log2f(Z)) * kLn2 : -INFINITY;
 }
 
 // Four groups where a thread would have many chunks and the CTAs leave SMs idle; at d = 64, where a group is two warps, for well more than it

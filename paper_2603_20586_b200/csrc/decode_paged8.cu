@@ -63,7 +63,8 @@ __device__ __forceinline__ float finite_abs(float x) {
     return a < INFINITY ? a : 0.f;                          // (NaN too)
 }
 // A partial's maximum and sum.  A score of NaN (a NaN among the row's keys or queries, or an infinite score) leaves NaN in the sum and in every
-// column; the combine kernel takes partials by "sum > 0", so such a one is made the largest, with an infinite sum: O is NaN, LSE infinite.
+// column; the combine kernel takes partials by "sum > 0", so such a one is made the largest, with an infinite sum: O is NaN, LSE infinite.  (Of several
+// tokens it ends as 0 and -infinity, as the tensor-core forward ends it.)
 __device__ __forceinline__ void put_max_sum(float* out, float m, float z) {
     const bool nan = !(z == z);
     out[0] = nan ? 1e38f : m;
@@ -613,10 +614,11 @@ __global__ void __launch_bounds__(W * 32, W == 4 ? 12 : 0) combine8_kernel(const
             }
         }
         Z = warp_sum(Z);
+        const bool some = Z > 0.f && !(p8.T > 0 && Z == INFINITY);                        // (several tokens: see DecodeParams::nan_is_none)
         __nv_bfloat16* const O = static_cast<__nv_bfloat16*>(p8.O) + row * DH;
 #pragma unroll
-        for (int i = 0; i < kCols; ++i) O[lane + 32 * i] = __float2bfloat16_rn(Z > 0.f ? A[i] / Z : 0.f);
-        if (p8.LSE && lane == 0) p8.LSE[row] = Z > 0.f ? (M + log2f(Z)) * kLn2 : -INFINITY;
+        for (int i = 0; i < kCols; ++i) O[lane + 32 * i] = __float2bfloat16_rn(some ? A[i] / Z : 0.f);
+        if (p8.LSE && lane == 0) p8.LSE[row] = some ? (M + log2f(Z)) * kLn2 : -INFINITY;
     }
 }
 template <int DH, int R, int W>
