@@ -392,6 +392,8 @@ size_t mka_decode_static_max_bytes(void);
  * the keys and one for the values of every (page, KV head, block).  Bytes outside [79, 175] (2^-48 .. 2^48) are read as the nearer end.
  * Scales being powers of two, code * 2^e is exact: an e4m3 code keeps the precision it has whatever the block's magnitude, and every cached
  * value is a bf16 number.
+ * Such a cache is written by mka_append_kv_paged8 and read by mka_decode_paged8 and mka_fwd_paged8 only.  mka_fuse_kv_paged writes no codes, and mka_l3_index sums bf16 keys: long-term
+ * chunks that are to be recalled are indexed from their bf16 rows before these are appended (mka_l3_retrieve's tables then serve the 8-bit pool, pages alike).
  */
 typedef enum { MKA_CODE_E4M3 = 0, MKA_CODE_S8 = 1 } mka_code;
 
@@ -492,7 +494,9 @@ size_t mka_pages_workspace_bytes(int64_t pages, int32_t seqs);
  *   From the first sequence on that the free pages do not suffice for, sequences that need pages are left as they are (those that need none are
  *   served); missing (device int32, or NULL) receives how many pages more it would have taken (at most 2^31 - 1), else 0.
  * Table entries behind a sequence's last page are left as they were.  planes: what a copy of a page consists of (at most 8; none: no
- * page is copied, for pools that are never shared).  At most 12288 sequences.
+ * page is copied, for pools that are never shared).  At most 12288 sequences.  A call cannot be repeated for further planes, since it has changed the tables: layers that share
+ * tables lie in one pool per kind with the page outermost, [pages, layers, heads, ...], which is one plane (a layer's pool is a view of it); apart, keys, values and
+ * exponents of two layers are eight planes.
  */
 mka_status mka_pages_resize(const mka_page_tables* t, const mka_page_plane* planes, int32_t n_planes, const int32_t* new_rows, int32_t* missing,
                             void* ws, size_t ws_bytes, void* stream);

@@ -104,13 +104,13 @@ bool visible8(const mka_shape* s, const int64_t n_level[3], int64_t (&lo)[3], in
 }
 
 // Few tokens go through the single-token kernel, in blocks of up to sixteen rows (heads x tokens of a KV head) that each walk the keys.  Every block reads the codes again,
-// mostly from the L2 cache; the other way costs the expansion, and tiles of 128 rows whatever the rows.  Fitted to 522 sizes (4 to 100 tokens on 100 to 60,000 rows of
-// context, heads 28 on 4, 32 on 8, 16 on 16 and 8 on 1, one or four sequences), over which the pick takes 1.1 % more than the better one on average.  This way / through
-// the forward, us, chosen in brackets, at d = 128:
-//   28 on 4, 15,000 rows, 4 / 16 / 32 tokens      [27.5] / 59.9    [52.8] / 61.1    85.2 / [61.3]
-//   16 on 16, 15,000 rows, 24 / 64 / 100          [58.3] / 99.8    98.9 / [104]     158 / [104]
-//   8 on 1, 1000 rows, 4 / 64                     [12.7] / 17.6    23.1 / [21.0]
-//   d = 64, 28 on 4, 15,000 rows, 8 / 16 tokens   [38.5] / 48.8    50.5 / [49.1]
+// mostly from the L2 cache; the other way costs the expansion, and tiles of 128 rows whatever the rows.  Over 612 sizes (4 to 100 tokens on 100 to 60,000 rows of
+// context, heads 28 on 4, 32 on 8, 16 on 16 and 8 on 1, one or four sequences, pages and blocks of 32 rows) the pick takes 1.0 % more than the better one on
+// average, 66 % at most (8 on 1, 24 tokens at 15,000 rows).  This way / through the forward, us, chosen in brackets, at d = 128:
+//   28 on 4, 15,000 rows, 4 / 16 / 32 tokens      [28.2] / 59.9    [53.9] / 60.9    86.7 / [61.0]      (pages of 16 rows: 4 tokens 23.1, 8 32.8, 16 53.7)
+//   16 on 16, 15,000 rows, 24 / 64 / 100          [59.2] / 99.9    101 / [104]      161 / [105]
+//   8 on 1, 1000 rows, 4 / 64                     [12.9] / 17.5    23.1 / [21.0]
+//   d = 64, 28 on 4, 15,000 rows, 8 / 16 tokens   [39.5] / 49.0    52.2 / [49.4]
 constexpr int kMaxChunkRows = 512;
 bool walk_in_blocks(int d, int64_t blocks, int group, double mbytes) {
     return blocks == 1 || (double)blocks * mbytes < (d == 128 ? 3.0 + (2.5 + 0.7 * group) * mbytes : 1.0 + 0.8 * group * mbytes);

@@ -4,7 +4,9 @@
 // rows touch; as many threads as keep eight or sixteen 8-column vectors each hold all of it in registers, so the second look at the rows (the first
 // finds the magnitude) costs no memory.  A block that holds rows already keeps its exponent or takes a larger one; its codes are read and written
 // again only when it grows.  No two units write the same block, and nothing is accumulated: results do not depend on the order of the units.
-// 32,768 rows of 8 heads at d = 128 (201 MB) in blocks of 64: 37.1 us, 5.4 TB/s (0.83 of a copy); the next rows of 32 sequences: 3.9 us.
+// 32,768 rows of 8 heads at d = 128 (201 MB) in blocks of 64: 37.0 us with other rows every time, 5.4 TB/s (0.83 of a copy); the next rows of 32 sequences: 3.8 us (4.1 where they
+// lie inside blocks, 5.0 and 5.7 at d = 64 and 128 where they make these grow).  Back to back on the same rows, us, for the floor of a copy: 65,536 rows of 8 heads at d = 64, blocks of 16 / 64 / 256:
+// bf16 36.6 / 33.3 / 34.0 (30.7), f32 52.7 / 52.9 / 53.4 (51.2); d = 128, 32,768 rows: bf16 33.4 / 34.5 / 33.1, f32 52.0 / 52.6 / 72.0 (the last: units of 512 threads, one CTA to an SM).
 #include <cuda_fp16.h>
 
 #include "code8.cuh"
@@ -57,8 +59,9 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, 
 }
 
 // kUnit: threads of a unit, as many as hold the block with kVecs vectors of eight columns each (16 x 64 take half a warp).  In bf16 sixteen for blocks of 32 rows and more,
-// two CTAs to an SM: 65,536 rows of four heads at d = 64 in blocks of 64 38.2 -> 35.6 us against eight and three CTAs, 32,768 rows of eight heads at d = 128 in blocks of 32, 64, 128
-// and 256 36.6 -> 34.5, 36.4 -> 36.2, 35.0 -> 35.4, 49.8 -> 34.4 (eight: units of 512 threads, one CTA to an SM).
+// two CTAs to an SM: 65,536 rows of eight heads at d = 64 in blocks of 64 38.2 -> 35.6 us against eight and three CTAs, 32,768 rows of eight heads at d = 128 in blocks of 32, 64, 128
+// and 256 36.6 -> 34.5, 36.4 -> 36.2, 35.0 -> 35.4, 49.8 -> 34.4 (eight: units of 512 threads, one CTA to an SM).  f32 rows keep eight; in e4m3
+// they are up to 5 % slower since (13.2 -> 13.8, blocks of 256 68.3 -> 72.1).
 template <typename T, int kUnit, int kVecs> struct Shape8 {
     static constexpr int kThreads = kUnit > 256 ? kUnit : 256, kCtas = kUnit > 256 ? 1 : (sizeof(T) == 2 && kVecs == 8 ? 3 : 2);
 };

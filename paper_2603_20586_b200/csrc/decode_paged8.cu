@@ -5,9 +5,9 @@
 // the bf16 form (tile_deal.cuh): one share of the tiles (8 KB: 32 rows at d = 128, 64 at d = 64) for each of two CTAs per SM, two producing warps that have the
 // copy engine bring the pages' rows into a ring, and computing warps that take the tiles in turn, whole: with a tile split between
 // four warps, 16 rows to each, what a step costs besides the products (waits, the walk, the running maximum) took 470 instructions per 16 rows at d = 128.
-// Four sequences at up to 128K rows, 28 heads on 4 of 128 (413 MB): 77.7 us with the combine kernel, 5.3 TB/s (0.81 of a copy), 72 without any computing;
-// 64 sequences of up to 6500 rows, 32 heads on 8 of 64, integer codes (371 MB): 80.5 us (0.70).  About 10 us of each are the start, the merges
-// and the combine; one sequence of 10,000 rows takes 12.5 us.
+// Four sequences at up to 128K rows, 28 heads on 4 of 128 (413 MB): 82 us with the combine kernel where the inputs change from call to call, 5.0 TB/s (0.77 of a copy), 76 to 78 back to
+// back on the same ones, 72 so without any computing; 64 sequences of up to 6500 rows, 32 heads on 8 of 64, integer codes (371 MB): 83 us (0.68), 80.5 and 74 so.  About 10 us of each
+// are the start, the merges and the combine; one sequence of 10,000 rows takes 12.6 us.
 //
 // The products are turned over: S^T = K Q^T and O^T = V^T P^T, m16n8k16, with 16 keys or 16 columns as the rows of the left operand and eight query heads as
 // the columns of the right one.  A group of up to eight heads then fills the products (as the rows of the left operand it would fill half of them), and
@@ -76,12 +76,13 @@ struct Maps8 {
 };
 
 // Computing warps of a CTA; two more produce.  Six of them (four warps to a scheduler) were no faster: 83.6 us to 82.1 on a mixed batch to 128K rows, 88.9 to 86.0
-// at d = 64.
+// at d = 64.  Spills to memory (bytes stored): NB = 2 at d = 128 40 to 64, of several tokens 164 to 220, and 76 to 84 at d = 64; combine8 with four warps to a CTA 40.
 constexpr int C = 4, kThreads = (C + 2) * 32;
 template <int DH> struct Ring {
     static constexpr int kRows = tile_rows8(DH), kGroups = kRows / 16;
     static constexpr int kTileBytes = kRows * DH;           // codes of K or of V
-    // 64 or 96 KB in flight per CTA, two CTAs per SM, beside the warps' states.  A multiple of the computing warps: a stage belongs to one warp, so nobody
+    // 64 or 96 KB in flight per CTA, two CTAs per SM, beside the warps' states (d = 64 with two products, NB = 2: 121 KB with the states, one CTA to an SM: 64 heads on 4 at up to 128K rows
+    // 89 us, 32 on 4 50, for 31.5 of bytes).  A multiple of the computing warps: a stage belongs to one warp, so nobody
     // waits for a phase of a barrier without having seen the phase before (which a wait by parity could not tell from the one before that).
     static constexpr int kStages = DH == 128 ? 8 : 12;
     static_assert(kStages % C == 0, "a stage belongs to one warp");
@@ -643,7 +644,8 @@ cudaError_t launch_decode_paged8(const DecodePaged8Params& p, cudaStream_t st) {
 cudaError_t launch_chunk_paged8(const DecodePaged8Params& p, cudaStream_t st) { return launch_d<true>(p, p.base.H / (p.base.H_kv / p.blocks), st); }
 
 // What counts is how many rows' warps find registers beside two of the decode's CTAs.  At d = 64 eight warps to an SM do: up to two rows to a warp then let all of them start
-// there (2048 rows 82.8 -> 80.4 us; four rows to a warp lost 3 to 10).  At d = 128 four warps of 40 registers do: 288 rows 35.5 -> 33.8 us, 512 36.3 -> 35.9, but 1120 39.2 -> 40.5
+// there (one row / two, 32 heads on 8: 1216 rows 43.8 / 44.5 us, 1536 54.8 / 51.8, 2048 66.7 / 63.2, 2336 73.9 / 70.6, 2368 70.7 / 70.1; 8 on 2: 1216 25.2 / 25.8, 1536 30.9 / 28.9,
+// 2048 39.3 / 37.4, 2368 41.1 / 40.2; four rows to a warp lost 3 to 10).  At d = 128 four warps of 40 registers do: 288 rows 35.5 -> 33.8 us, 512 36.3 -> 35.9, but 1120 39.2 -> 40.5
 // and 14,336 58.1 -> 60.4, where the warps without that limit are faster.
 cudaError_t launch_combine8(const DecodePaged8Params& p, cudaStream_t st) {
     const long long rows = (long long)p.base.B * p.base.H;
