@@ -439,6 +439,8 @@ mka_status mka_append_kv_paged8(int32_t B, int32_t H, int64_t n, int32_t d, int3
  * value block's scale) is off by 2^-11 of itself, and by 2^-34 of the largest such product of the row; where the exponents of the value blocks lie D > 91 apart, by
  * 2^(D - 125) of it, 2^-29 at most: far below what a rounding of that block's codes makes.
  * A NaN among a sequence's valid keys, or an infinite score, gives NaN in O (LSE +inf).
+ * bf16 and MKA_MODE_FAST only, here and in mka_fwd_paged8: f32, MKA_MODE_FULL and MKA_FLAG_FORCE_SIMT return MKA_ERR_UNSUPPORTED (there is no form with fp32 weights), and so do levels of
+ * different codes.
  * With t = the tiles (32 rows, 64 at d = 64) of a sequence of n rows on every level, t * B, t * H_kv and t * B * H_kv / 296 must fit 31 bits (MKA_ERR_SHAPE).
  *   ws: mka_decode_paged8_workspace_bytes(shape, H_kv, n_level) bytes, 4-byte aligned; first word: the device status (bounded waits as in
  *       mka_decode_paged)

@@ -201,22 +201,31 @@ def _stream(stream) -> int:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
 
 
+def _handle(stream) -> int:
+    h = stream.cuda_stream
+    return getattr(h, "value", h) or 0                                       # (a c_void_p is taken too)
+
+
+def _other(stream) -> bool:
+    """Whether the call's stream is another one than torch's current one."""
+    return stream is not None and _handle(stream) != _stream(None)
+
+
 def _torch_stream(stream, device):
-    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device)
+    return stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_handle(stream), device)
 
 
 def _on(stream, *own):
     """Tensors that a call made on torch's current stream for its work on another one: when they are dropped, their memory is not given out again before
     that stream is done with them."""
-    if stream is not None:
-        for t in own:
-            if t is not None and t.is_cuda:
-                t.record_stream(_torch_stream(stream, t.device))
+    for t in own:
+        if t is not None and t.is_cuda and _other(stream):
+            t.record_stream(_torch_stream(stream, t.device))
 
 
 def _scratch(nbytes: int, device, stream) -> torch.Tensor:
     """nbytes of torch's memory on the call's stream, to which it goes back when the call has been queued there."""
-    if stream is None or torch.device(device).type != "cuda":
+    if torch.device(device).type != "cuda" or not _other(stream):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
     with torch.cuda.stream(_torch_stream(stream, device)):
         return torch.empty(nbytes, dtype=torch.uint8, device=device)

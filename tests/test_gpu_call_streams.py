@@ -1,5 +1,7 @@
 """Calls on a stream of their own, beside torch's current one: what a call allocates (outputs that the caller drops, workspaces) is not handed out again before
 that stream is done with it."""
+import ctypes
+
 import pytest
 import torch
 
@@ -83,3 +85,26 @@ def test_dropped_memory_is_not_handed_out_early(mka, name):
     assert not stream.query()
     torch.cuda.synchronize()
     assert bool((torch.stack(taken) == 0x5a).all()), name
+
+
+class Handle:
+    """What has a cuda_stream is a stream: a number, or a c_void_p."""
+
+    def __init__(self, value):
+        self.cuda_stream = value
+
+
+@pytest.mark.parametrize("wrap", [int, ctypes.c_void_p])
+@pytest.mark.parametrize("name", ["decode", "fwd_paged", "decode_paged8", "fwd_paged8", "compact"])
+def test_streams_of_other_kinds(mka, name, wrap):
+    call = calls(mka)[name]
+    want, stream = call(None), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    if name == "compact":                                        # (nothing moves the second time)
+        want = call(None)
+        torch.cuda.synchronize()
+    for s in (Handle(wrap(stream.cuda_stream)), Handle(wrap(torch.cuda.current_stream().cuda_stream))):
+        got = call(s)
+        torch.cuda.synchronize()
+        pairs = zip(want, got) if isinstance(want, tuple) else [(want, got)]
+        assert all(torch.equal(a, b) for a, b in pairs)
